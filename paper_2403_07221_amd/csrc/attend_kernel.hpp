@@ -16,30 +16,10 @@
 
 #include <type_traits>
 
+#include "attend_tile.hpp"
 #include "elem16.hpp"
 
 namespace lffn {
-
-struct AttendArgs {
-    const void *q;
-    void *y;
-    const uint8_t *k_cache, *v_cache;
-    const float *k_scale, *v_scale;
-    const int *table, *starts, *lengths;
-    bool join_each;       // the join takes several rows to a workgroup
-    float *part;          // [chunk][token * heads][dim]: sums of a chunk of keys, of tiles whose keys take several; null where none does
-    float *part_ml;       // [chunk][token * heads][2]: its maximum (in powers of two) and its sum of probabilities
-    long long q_token, q_head, y_token, y_head, table_stride;
-    int n_tokens, requests, heads, kv_heads, group;
-    unsigned group_inverse;   // floor(2^32 / group), for group > 1
-    int width, n_blocks, block_log;
-    int causal, window, max_keys;
-    int max_queries;      // tokens of a request that the grid (and the few-row kernel's LDS) has room for
-    int chunk, chunks;    // keys of a chunk, chunks of the grid
-    int row_tiles;        // tiles of rows of a request and key head, of the grid
-    int tile_rows;        // rows of a tile
-    float scale;          // log2(e) / sqrt(dim)
-};
 
 typedef float fv4 __attribute__((ext_vector_type(4)));
 typedef unsigned uv4 __attribute__((ext_vector_type(4)));
@@ -61,57 +41,6 @@ __device__ __forceinline__ hf8 widen8_half(unsigned lo, unsigned hi)
     const hf2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, true);
     const hf2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, false), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, true);
     return hf8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
-}
-
-// The rows that a workgroup has and the keys they see.
-struct RowTile {
-    int r, h;                 // request, key head
-    int first, fresh, past;   // the request's first token and its tokens; the position of the first
-    int row0, rows;           // first row of the tile; rows of the request
-    int lo, hi;               // keys that some row sees: lo .. hi - 1
-};
-
-// the query that a row belongs to: row / group (the product falls short of it by one at most)
-__device__ __forceinline__ int query_of(const AttendArgs &a, int row)
-{
-    if (a.group == 1) return row;
-    const unsigned q = __umulhi((unsigned)row, a.group_inverse);
-    return (int)(q + ((unsigned)row - q * (unsigned)a.group >= (unsigned)a.group));
-}
-
-__device__ __forceinline__ RowTile row_tile(const AttendArgs &a, int combo, int tile, int tile_rows)
-{
-    RowTile t;
-    t.r = combo / a.kv_heads;
-    t.h = combo - t.r * a.kv_heads;
-    t.first = min(max(a.starts[t.r], 0), a.n_tokens);
-    t.fresh = min(max(a.starts[t.r + 1], t.first), a.n_tokens) - t.first;
-    const long long held = (long long)a.width << a.block_log;
-    const int length = min(max(a.lengths[t.r], 0), (int)min(held, (long long)a.max_keys));
-    t.past = max(a.lengths[t.r], 0) - t.fresh;
-    t.rows = min(t.fresh, a.max_queries) * a.group;
-    t.row0 = tile * tile_rows;
-    const int i0 = query_of(a, t.row0), i1 = query_of(a, max(min(t.row0 + tile_rows, t.rows) - 1, 0));
-    t.hi = a.causal ? max(min(length, t.past + i1 + 1), 0) : length;
-    t.lo = a.window ? max(t.past + i0 - a.window + 1, 0) : 0;
-    t.lo &= ~63;   // chunks and steps begin at multiples of 64 keys
-    return t;
-}
-
-// the keys lo .. hi - 1 that row `row` of the tile's request sees
-__device__ __forceinline__ void row_keys(const AttendArgs &a, const RowTile &t, int row, int &lo, int &hi)
-{
-    const int i = query_of(a, row);
-    hi = a.causal ? min(t.hi, t.past + i + 1) : t.hi;
-    lo = a.window ? max(t.past + i - a.window + 1, 0) : 0;
-}
-
-// The block that holds a request's keys from `key` on, in two steps so that the first's load can be long on its way before the second:
-// what the table says, and that or -1 where the table, or the keys before `end`, or the cache have no such block.
-__device__ __forceinline__ int table_entry(const AttendArgs &a, const int *row, int key) { return row[min(key >> a.block_log, a.width - 1)]; }
-__device__ __forceinline__ int block_of(const AttendArgs &a, int entry, int key, int end)
-{
-    return key < end && (key >> a.block_log) < a.width && entry >= 0 && entry < a.n_blocks ? entry : -1;
 }
 
 template <int KIND>
@@ -230,7 +159,8 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 2 : 1) void attend_few_kernel(Att
     if (chunk >= a.chunks) return;
     const RowTile t = row_tile(a, combo, tile, ROWS);
     if (t.row0 >= t.rows) return;
-    const int c0 = t.lo + chunk * a.chunk, c1 = min(t.hi, c0 + a.chunk);   // (lo + chunks * chunk stays far below 2^31)
+    int c0, c1;
+    chunk_keys(a, t, chunk, c0, c1);
     if (c0 >= c1 && chunk > 0) return;
     // one chunk has all the tile's keys (or there are none, or the grid, for requests that bring more than max_queries): y is written here
     const bool whole = t.hi - t.lo <= a.chunk || a.chunks == 1;
@@ -540,7 +470,8 @@ __global__ __launch_bounds__(256, KIND != kElemF32 && DIM <= 128 ? 2 : 1) void a
     const int tile = a.row_tiles - 1 - ((int)rest - chunk * a.row_tiles);
     const RowTile t = row_tile(a, combo, tile, ROWS);
     if (t.row0 >= t.rows) return;
-    const int c0 = t.lo + chunk * a.chunk, c1 = min(t.hi, c0 + a.chunk);
+    int c0, c1;
+    chunk_keys(a, t, chunk, c0, c1);
     if (c0 >= c1 && chunk > 0) return;
     // one chunk has all the tile's keys (or there are none, or the grid, for requests that bring more than max_queries): y is written here
     const bool whole = t.hi - t.lo <= a.chunk || a.chunks == 1;
