@@ -736,11 +736,11 @@ __global__ __launch_bounds__(256, KIND != kElemF32 && DIM <= 128 ? 2 : 1) void a
                     for (int n = 0; n < NP; ++n) o[d] = VO::mma(v8, p[u][n], o[d]);
                 }
     };
-    // the sums of rows that see a NaN value
+    // the sums of rows that see a NaN value, of the steps whose NaN bytes stage() has cleared: also for waves whose rows see all of the step
     auto nan_rows = [&](int buffer, int step) {
         const int key0 = c0 + step * kManyKeys;
         const unsigned there = there_of(step);
-        if (!masked(key0, there)) return;
+        if (!edge(key0) && there == 15u) return;
         unsigned some_nan = 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) some_nan |= nans[buffer][i];
