@@ -331,7 +331,9 @@ int lookupffn_rotate_append(const void *q, const void *k, const void *v, const f
  * is not in the cache (a table entry outside 0 .. n_blocks - 1, or past the table) is not seen.  Values and keys that a row does not see
  * do not reach it, whatever they hold.  max_queries and max_keys bound the tokens that a request brings and the lengths (what goes beyond
  * is left out); they shape the launch, so tight ones are faster.
- * Sums, maximum and softmax are fp32; probabilities keep 11 bits or more (fp32 rows: 24) in the product with the values.
+ * Sums, maximum and softmax are fp32; probabilities keep 11 bits or more (fp32 rows: 24) in the product with the values, those below 2^-22 of
+ * the row's largest what 11 bits there keep (2^-33).  Scales may be any floats; powers of two at most 2^8 apart, as rotate_append writes them for
+ * rows of like sizes, are the fastest.
  * strides: q, y.  dim 64, 128, 192 or 256.  Scratch: lookupffn_workspace_bytes_attend() bytes (0: the call needs none).
  */
 int lookupffn_attend(const void *q, const void *k_cache, const void *v_cache, const float *k_scale, const float *v_scale,

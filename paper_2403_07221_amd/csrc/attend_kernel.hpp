@@ -388,20 +388,28 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 2 : 1) void attend_few_kernel(Att
 
 // Many rows: prompts and encodings.  A workgroup has 128 rows of one request and key head, a wave 32 (KS = 2: 64, and of a step's two tiles
 // of 32 keys each wave has one; two waves join at the end); its keys go through LDS in steps of 64, widened to the matrix cores' type once
-// for all four waves.  Measured: 4 prompts of 3500 to 4096 tokens, 32 heads on 8 of 128, 606 us, 800 TFLOP/s; 64 encodings of 300 to 512,
-// 12 heads of 64, 77 us, 460 TFLOP/s; 24 requests with 3 to 8 drafted tokens, 16 heads on 2 of 256 (KS = 2), 49 us, 1.1 TB/s.
+// for all four waves.  Measured: 4 prompts of 3500 to 4096 tokens, 32 heads on 8 of 128, 600 us, 810 TFLOP/s; 64 encodings of 300 to 512,
+// 12 heads of 64, 77 us, 460 TFLOP/s; 24 requests with 3 to 8 drafted tokens, 16 heads on 2 of 256 (KS = 2), 46 us, 1.2 TB/s.
 //
 // What bounds it: the matrix cores, and beside them the softmax's vector instructions.  Scores are S^T = K Q^T in tiles of 32 keys x 32
 // rows, so a row's probabilities lie along a lane column, and as they stand they are the right operand of y^T = V^T P^T: a lane half h
 // holds keys 16 u + 8 h .. + 7 of the tile's step u because row m of the tile stands for key m with its bits 2 and 3 exchanged.
 //
 // Scales cost no instruction for each score: they are powers of two as rotate_append writes them, so the widening multiplies by the
-// block's scale relative to the largest of the chunk, exactly unless a block's scale is 2^-15 of it, where half loses bits that the
-// chunk's other scores, or values, do not have either.  What is left of a scale that is no power of two multiplies its keys' scores and
-// their probabilities, in steps that have such a scale.  Probabilities of 16-bit rows are half (11 bits, a relative 2^-12 each, as fine as
-// the finest 16-bit output) times 2^8, so that those of 2^-22 still have all their bits; fp32 rows keep three bf16 pieces (24 bits).
+// block's scale relative to the largest of the chunk.  That is exact down to 2^-15 (the smallest byte is 2^-9, half's smallest number
+// 2^-24), and is done down to 2^-kSpread.  Probabilities of 16-bit rows are half there (11 bits, off by a relative 2^-11 at most, as fine as
+// the finest 16-bit output) times 2^8, so that those of 2^-22 still have all their bits and smaller ones are off by 2^-33 at most; fp32 rows
+// keep three bf16 pieces (24 bits).
+//
+// A chunk with a scale that is no power of two, or with scales further apart, is `exact`: its bytes stay as they are, a block's scale
+// multiplies its fp32 scores or its fp32 probabilities, and those are two bf16 pieces (16-bit rows), as in the few-row kernel.  So no block's
+// scale costs the bits of another's bytes, and nothing of a block reaches a row that does not see it.  All of its steps cost what that takes:
+// the prompts above 1010 us, the encodings 153, the drafted tokens 58.
 constexpr int kManyKeys = 64;
 constexpr float kProbUp = 8.0f;   // probabilities times 2^8
+// Scales of a chunk lie at most 2^8 apart: 8192 probabilities off by 2^-33 each, of values 2^8 times the row's others, are then no more than
+// the rounding of one probability.
+constexpr int kSpread = 8;
 
 constexpr int kManyChunk = 8192;  // the most keys of a chunk: its segments lie in LDS
 constexpr int kManySegments = kManyChunk / 16 + 16;   // and some past the last
@@ -439,8 +447,15 @@ struct Operand<true> {
 };
 
 __device__ __forceinline__ float pow2f(int e) { return __uint_as_float((unsigned)(min(max(e, -126), 127) + 127) << 23); }
-// the exponent of a scale, and what is left of the scale (1 where it is a power of two)
-__device__ __forceinline__ int scale_exponent(float s) { return max((int)((__float_as_uint(s) >> 23) & 255u), 1) - 127; }
+__device__ __forceinline__ bool power_of_two(float s)   // 2^-126 .. 2^127
+{
+    const unsigned u = __float_as_uint(s);
+    return (u & 0x807FFFFFu) == 0 && u >= 0x00800000u && u < 0x7F800000u;
+}
+__device__ __forceinline__ int exponent_of(float s) { return (int)((__float_as_uint(s) >> 23) & 255u) - 127; }
+typedef short sv2 __attribute__((ext_vector_type(2)));
+
+#define LFFN_INLINE __attribute__((always_inline))   // (a lambda that both kinds of chunks call would keep its sums in memory)
 
 __device__ __forceinline__ float lane_of(float x, int lane)
 {
@@ -448,21 +463,25 @@ __device__ __forceinline__ float lane_of(float x, int lane)
 }
 
 template <int KIND, int DIM, int KS>
-__global__ __launch_bounds__(256, KIND != kElemF32 && DIM <= 128 ? 2 : 1) void attend_many_kernel(AttendArgs a)
+__global__ __launch_bounds__(256, KIND == kElemF32 || DIM > 128 ? 1 : DIM == 64 ? 3 : 2) void attend_many_kernel(AttendArgs a)
 {
     using Shape = ManyShape<KIND, DIM>;
     using KO = Operand<KIND == kElemF16>;     // keys and queries
     using VO = Operand<KIND != kElemF32>;     // values and probabilities
-    constexpr int NQ = QueryPieces<KIND>::N, NP = KIND == kElemF32 ? 3 : 1, ROWS = 128 / KS, KP = Shape::KP, VP = Shape::VP;
+    using XO = Operand<false>;                // those of an exact chunk
+    constexpr int NQ = QueryPieces<KIND>::N, NP = KIND == kElemF32 ? 3 : 1, XP = KIND == kElemF32 ? 3 : 2;   // pieces
+    constexpr int ROWS = 128 / KS, KP = Shape::KP, VP = Shape::VP;
     constexpr int T = 2 / KS;                 // tiles of 32 keys that a wave has of a step
     constexpr int PIECES = DIM / 64;          // 16-byte pieces of keys, and of values, that a thread stages
-    constexpr int FIRST = DIM == 64 ? 4 : 8;
+    // LDS reads ahead of the products.  Of 256 columns more than two leave too few registers, and the compiler drops the order: 8 prompts of 447 to
+    // 895 tokens after 134 to 404, 6 heads on 2 of 256, 72 us, with eight 79; 24 requests with 3 to 8 drafted tokens, 16 heads on 2, 46 and 47.
+    constexpr int FIRST = DIM == 64 ? 4 : DIM == 256 ? 2 : 8;
     constexpr float kNone = -__builtin_huge_valf();
     extern __shared__ uint16_t many_lds[];
     __shared__ uint64_t nan_keys[2][DIM];   // of a step that some row sees in part: the keys whose value is NaN in a column
     __shared__ uint32_t nans[2][4];        // whether a wave has staged any
     __shared__ uv2 segments[kManySegments];       // block or -1; the upper halves of the keys' and the values' relative scale
-    __shared__ int tops[4][3];
+    __shared__ int tops[4][3];   // of a wave's segments: the largest exponents, the smallest negated, whether some scale is no power of two
     const unsigned wg = blockIdx.y * gridDim.x + blockIdx.x, combos = (unsigned)(a.requests * a.kv_heads), rest = wg / combos;
     const int combo = (int)(wg - rest * combos), chunk = (int)(rest / (unsigned)a.row_tiles);
     if (chunk >= a.chunks) return;
@@ -515,51 +534,54 @@ __global__ __launch_bounds__(256, KIND != kElemF32 && DIM <= 128 ? 2 : 1) void a
     const long long head_bytes = (long long)DIM << a.block_log;
 
     const int steps = c0 < c1 ? (c1 - c0 + kManyKeys - 1) / kManyKeys : 0;
-    // The chunk's segments of 16 keys, all looked up before the first step: their blocks, and their scales relative to the powers of two
-    // that the largest have.
-    float k_unit, v_unit;   // those powers
-    bool left;              // some segment has something left beside its power of two
+    // The chunk's segments of 16 keys, all looked up before the first step: their blocks, and their scales relative to the largest
+    // (as they are, in an exact chunk).
+    float k_unit = 1.0f, v_unit = 1.0f;   // what the largest are
+    bool exact;
     {
-        int k_top = -200, v_top = -200;
+        sv2 top = {-300, -300}, low = top;   // exponents of keys' and values' scales, and those negated
         bool odd = false;
         for (int i = tid; i < 4 * (steps + 1); i += 256) {
             const int key = c0 + 16 * i, id = a.width ? block_of(a, table_entry(a, table, key), key, c1) : -1;
             const long long at = (long long)max(id, 0) * a.kv_heads + t.h;
-            const float ks = id >= 0 ? a.k_scale[at] : 0.0f, vs = id >= 0 ? a.v_scale[at] : 0.0f;
-            const int ek = scale_exponent(ks), ev = scale_exponent(vs);
-            const float kl = id >= 0 ? ks * pow2f(-ek) : 1.0f, vl = id >= 0 ? vs * pow2f(-ev) : 1.0f;
+            const float ks = id >= 0 ? a.k_scale[at] : 1.0f, vs = id >= 0 ? a.v_scale[at] : 1.0f;
+            const int ek = exponent_of(ks), ev = exponent_of(vs);
             segments[i] = uv2{(unsigned)id, (unsigned)(ek + 256) << 16 | (unsigned)(ev + 256)};
-            odd |= kl != 1.0f || vl != 1.0f;
-            k_top = id >= 0 ? max(k_top, ek) : k_top;
-            v_top = id >= 0 ? max(v_top, ev) : v_top;
+            odd |= !power_of_two(ks) || !power_of_two(vs);
+            if (id >= 0) {
+                top = __builtin_elementwise_max(top, sv2{(short)ek, (short)ev});
+                low = __builtin_elementwise_max(low, sv2{(short)-ek, (short)-ev});
+            }
         }
         for (int d = 1; d < 64; d <<= 1) {
-            k_top = max(k_top, __shfl_xor(k_top, d));
-            v_top = max(v_top, __shfl_xor(v_top, d));
+            top = __builtin_elementwise_max(top, __builtin_bit_cast(sv2, __shfl_xor(__builtin_bit_cast(int, top), d)));
+            low = __builtin_elementwise_max(low, __builtin_bit_cast(sv2, __shfl_xor(__builtin_bit_cast(int, low), d)));
         }
         const int any = __any(odd);
         if (lane == 0) {
-            tops[w][0] = k_top;
-            tops[w][1] = v_top;
+            tops[w][0] = __builtin_bit_cast(int, top);
+            tops[w][1] = __builtin_bit_cast(int, low);
             tops[w][2] = any;
         }
         __syncthreads();
-        int any_left = 0;
+        int any_odd = 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            k_top = max(k_top, tops[i][0]);
-            v_top = max(v_top, tops[i][1]);
-            any_left |= tops[i][2];
+            top = __builtin_elementwise_max(top, __builtin_bit_cast(sv2, tops[i][0]));
+            low = __builtin_elementwise_max(low, __builtin_bit_cast(sv2, tops[i][1]));
+            any_odd |= tops[i][2];
         }
-        k_top = __builtin_amdgcn_readfirstlane(k_top);
-        v_top = __builtin_amdgcn_readfirstlane(v_top);
-        left = __builtin_amdgcn_readfirstlane(any_left) != 0;
-        k_unit = pow2f(k_top);
-        v_unit = pow2f(v_top);
+        const int k_top = __builtin_amdgcn_readfirstlane(top[0]), v_top = __builtin_amdgcn_readfirstlane(top[1]);
+        exact = __builtin_amdgcn_readfirstlane(any_odd != 0 || k_top + low[0] > kSpread || v_top + low[1] > kSpread) != 0;
+        if (!exact) {
+            k_unit = pow2f(k_top);
+            v_unit = pow2f(v_top);
+        }
         for (int i = tid; i < 4 * (steps + 1); i += 256) {
             const uv2 e = segments[i];
-            // (bytes that stand in for a block that is not there become zeros)
-            segments[i][1] = (int)e[0] < 0 ? 0u : __float_as_uint(pow2f((int)(e[1] >> 16) - 256 - k_top)) | __float_as_uint(pow2f((int)(e[1] & 0xFFFFu) - 256 - v_top)) >> 16;
+            const unsigned rel = __float_as_uint(pow2f((int)(e[1] >> 16) - 256 - k_top)) | __float_as_uint(pow2f((int)(e[1] & 0xFFFFu) - 256 - v_top)) >> 16;
+            // (bytes that stand in for a block that is not there become zeros, or all but)
+            segments[i][1] = (int)e[0] < 0 ? 0u : exact ? 0x3F803F80u : rel;
         }
         __syncthreads();
     }
@@ -572,7 +594,7 @@ __global__ __launch_bounds__(256, KIND != kElemF32 && DIM <= 128 ? 2 : 1) void a
     const unsigned block_bytes = (unsigned)(a.kv_heads * head_bytes);
     const uint8_t *k_head = a.k_cache + t.h * head_bytes, *v_head = a.v_cache + t.h * head_bytes + ((long long)v_column << a.block_log);
     auto segment = [&](int step) { return segments[4 * step + (lane & 3)]; };   // of this lane
-    auto fetch = [&](int step, const uv2 &e) {
+    auto fetch = [&](int step, const uv2 &e) LFFN_INLINE {
         const int key0 = c0 + step * kManyKeys, id = max((int)e[0], 0);
         const uint8_t *kp = k_head + (unsigned long long)(unsigned)__builtin_amdgcn_readlane(id, w) * block_bytes + ((key0 + 16 * w) & in_block) * DIM;
         const uint8_t *vp = v_head + (unsigned long long)(unsigned)id * block_bytes + ((key0 + seg16) & in_block);
@@ -582,18 +604,8 @@ __global__ __launch_bounds__(256, KIND != kElemF32 && DIM <= 128 ? 2 : 1) void a
             vr[p] = *reinterpret_cast<const uv4 *>(vp + (64 * p << a.block_log));
         }
     };
-    // what is left of a block's scale beside its power of two
-    auto left_of = [&](const float *scale, int id) {
-        const float s = id >= 0 ? scale[(long long)id * a.kv_heads + t.h] : 1.0f;
-        return s * pow2f(-scale_exponent(s));
-    };
-    auto stage = [&](int buffer, int step, const uv2 &e) {   // e: segment(step), as it was fetched
+    auto stage = [&](auto exactly, int buffer, int step, const uv2 &e) LFFN_INLINE {   // e: segment(step), as it was fetched
         const bool there = (int)e[0] >= 0;
-        // values whose scale is not finite are NaN, so that only the rows that see them get one
-        if (left && !(fabsf(left_of(a.v_scale, (int)e[0])) < __uint_as_float(0x7F800000u))) {
-#pragma unroll
-            for (int p = 0; p < PIECES; ++p) vr[p] = uv4{0x7F7F7F7Fu, 0x7F7F7F7Fu, 0x7F7F7F7Fu, 0x7F7F7F7Fu};
-        }
         // Steps that some row sees in part: a masked key's probability is zero, but zero times a NaN byte is not.  Such bytes become
         // zeros, and their places go to the rows that do see them.
         if (edge(c0 + step * kManyKeys) || __any(!there)) {
@@ -622,9 +634,10 @@ __global__ __launch_bounds__(256, KIND != kElemF32 && DIM <= 128 ? 2 : 1) void a
             typename KO::V *to = reinterpret_cast<typename KO::V *>(kb + key * KP + column);
             to[0] = KO::widen(kr[p][0], kr[p][1], fk);
             to[1] = KO::widen(kr[p][2], kr[p][3], fk);
-            typename VO::V *tv = reinterpret_cast<typename VO::V *>(vb + (v_column + 64 * p) * VP + seg16);
-            tv[0] = VO::widen(vr[p][0], vr[p][1], fv);
-            tv[1] = VO::widen(vr[p][2], vr[p][3], fv);
+            using O = std::conditional_t<decltype(exactly)::value, XO, VO>;
+            typename O::V *tv = reinterpret_cast<typename O::V *>(vb + (v_column + 64 * p) * VP + seg16);
+            tv[0] = O::widen(vr[p][0], vr[p][1], fv);
+            tv[1] = O::widen(vr[p][2], vr[p][3], fv);
         }
     };
 
@@ -633,7 +646,7 @@ __global__ __launch_bounds__(256, KIND != kElemF32 && DIM <= 128 ? 2 : 1) void a
     auto there_of = [&](int step) { return (unsigned)__ballot((int)segment(step)[0] >= 0) & 15u; };
     auto masked = [&](int key0, unsigned there) { return key0 < all_lo || key0 + kManyKeys > all_hi || there != 15u; };
     // the keys of a step that a row sees, a bit each
-    auto seen_keys = [&](int key0, unsigned there) {
+    auto seen_keys = [&](int key0, unsigned there) LFFN_INLINE {
         int lo = key_lo, hi = key_hi;
         asm volatile("" : "+v"(lo), "+v"(hi));   // (not to be worked out in the steps without a mask)
         const int from = min(max(lo - key0, 0), 64), to = min(max(min(hi, c1) - key0, 0), 64);
@@ -643,7 +656,7 @@ __global__ __launch_bounds__(256, KIND != kElemF32 && DIM <= 128 ? 2 : 1) void a
         return from == 64 ? 0 : below & (~0ull << from) & in;
     };
     fv16 s[T];
-    auto scores = [&](int buffer) {
+    auto scores = [&](int buffer) LFFN_INLINE {
         const uint16_t *kb = many_lds + buffer * Shape::BUFFER;
 #pragma unroll
         for (int tt = 0; tt < T; ++tt) s[tt] = fv16{};
@@ -657,26 +670,33 @@ __global__ __launch_bounds__(256, KIND != kElemF32 && DIM <= 128 ? 2 : 1) void a
             }
     };
     const float unit = k_unit * a.scale;
-    typename VO::V p[2 * T][NP];   // [16 keys of the wave's tiles]
-    auto softmax = [&](int step) {
+    // the scale of the block of segment u of the wave's tiles
+    auto scale_of_segment = [&](const float *scale, int step, int u) {
+        const int id = (int)segments[4 * step + 2 * tile0 + u][0];
+        return id >= 0 ? scale[(long long)id * a.kv_heads + t.h] : 1.0f;
+    };
+    auto softmax = [&](auto exactly, int step, auto &p) LFFN_INLINE {   // p: pieces of the probabilities, of 16 keys of the wave's tiles each
+        constexpr bool EXACT = decltype(exactly)::value;
         const int key0 = c0 + step * kManyKeys;
         const unsigned there = there_of(step);
-        if (left) {
+        if constexpr (EXACT) {
 #pragma unroll
             for (int u = 0; u < 2 * T; ++u) {
-                const float k_left = left_of(a.k_scale, (int)segments[4 * step + 2 * tile0 + u][0]);
+                const float ks = scale_of_segment(a.k_scale, step, u);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) s[u >> 1][8 * (u & 1) + e] *= k_left;
+                for (int e = 0; e < 8; ++e) s[u >> 1][8 * (u & 1) + e] *= ks;
             }
         }
-        if (masked(key0, there)) {
+        const bool partly = masked(key0, there);
+        unsigned words[T];   // bit 16 (e / 8) + e % 8 of word tt: whether the row sees the key of s[tt][e]
+        if (partly) {
             const uint64_t seen = seen_keys(key0, there);
 #pragma unroll
             for (int tt = 0; tt < T; ++tt) {
-                const unsigned word = (unsigned)(seen >> (32 * (tile0 + tt))) >> (8 * h);
+                words[tt] = (unsigned)(seen >> (32 * (tile0 + tt))) >> (8 * h);
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
-                    if (!(word & (1u << (16 * (e >> 3) + (e & 7))))) s[tt][e] = kNone;
+                    if (!(words[tt] & (1u << (16 * (e >> 3) + (e & 7))))) s[tt][e] = kNone;
             }
         }
         float top = kNone;
@@ -693,37 +713,39 @@ __global__ __launch_bounds__(256, KIND != kElemF32 && DIM <= 128 ? 2 : 1) void a
             for (int d = 0; d < DIM / 32; ++d) o[d] *= down;
             m = now;
         }
-        const float base = (m == kNone ? 0.0f : m) - kProbUp;
+        const float base = (m == kNone ? 0.0f : m) - (EXACT ? 0.0f : kProbUp);
 #pragma unroll
         for (int tt = 0; tt < T; ++tt)
 #pragma unroll
             for (int e = 0; e < 16; ++e) s[tt][e] = __builtin_amdgcn_exp2f(fmaf(s[tt][e], unit, -base));
-        auto pieces = [&](auto with_left) {
 #pragma unroll
-            for (int u = 0; u < 2 * T; ++u) {
-                float v_left = decltype(with_left)::value ? left_of(a.v_scale, (int)segments[4 * step + 2 * tile0 + u][0]) : 1.0f;
-                v_left = fabsf(v_left) < __uint_as_float(0x7F800000u) ? v_left : 1.0f;   // (NaN since it was staged)
+        for (int u = 0; u < 2 * T; ++u) {
+            float vs = 1.0f;
+            if constexpr (EXACT) vs = scale_of_segment(a.v_scale, step, u);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    float rest = s[u >> 1][8 * (u & 1) + e];
-                    if (decltype(with_left)::value) rest *= v_left;
+            for (int e = 0; e < 8; ++e) {
+                float rest = s[u >> 1][8 * (u & 1) + e];
+                if constexpr (EXACT) {
+                    rest *= vs;
+                    if (partly) rest = words[u >> 1] & (1u << (16 * (u & 1) + e)) ? rest : 0.0f;   // (a scale that the row does not see may be anything)
+                }
+                constexpr int N = EXACT ? XP : NP;
 #pragma unroll
-                    for (int n = 0; n < NP; ++n) {
-                        p[u][n][e] = rest;
-                        if (n + 1 < NP) rest -= (float)p[u][n][e];
-                    }
+                for (int n = 0; n < N; ++n) {
+                    p[u][n][e] = rest;
+                    if (n + 1 < N) rest -= (float)p[u][n][e];
                 }
             }
-        };
-        pieces(std::false_type{});
+        }
         // (the sum is of the probabilities as they are, not as they were rounded)
 #pragma unroll
         for (int tt = 0; tt < T; ++tt)
 #pragma unroll
             for (int e = 0; e < 16; ++e) l += s[tt][e];
-        if (left) pieces(std::true_type{});
     };
-    auto sums = [&](int buffer) {
+    auto sums = [&](auto exactly, int buffer, const auto &p) LFFN_INLINE {
+        using O = std::conditional_t<decltype(exactly)::value, XO, VO>;
+        constexpr int N = decltype(exactly)::value ? XP : NP;
         const uint16_t *vb = many_lds + buffer * Shape::BUFFER + kManyKeys * KP;
 #pragma unroll
         for (int d2 = 0; d2 < DIM / 32; d2 += 2)   // (two sums in turn)
@@ -731,13 +753,13 @@ __global__ __launch_bounds__(256, KIND != kElemF32 && DIM <= 128 ? 2 : 1) void a
             for (int u = 0; u < 2 * T; ++u)
 #pragma unroll
                 for (int d = d2; d < d2 + 2; ++d) {
-                    const typename VO::V v8 = *reinterpret_cast<const typename VO::V *>(vb + (32 * d + lr) * VP + 32 * tile0 + 16 * u + 8 * h);
+                    const typename O::V v8 = *reinterpret_cast<const typename O::V *>(vb + (32 * d + lr) * VP + 32 * tile0 + 16 * u + 8 * h);
 #pragma unroll
-                    for (int n = 0; n < NP; ++n) o[d] = VO::mma(v8, p[u][n], o[d]);
+                    for (int n = 0; n < N; ++n) o[d] = O::mma(v8, p[u][n], o[d]);
                 }
     };
     // the sums of rows that see a NaN value, of the steps whose NaN bytes stage() has cleared: also for waves whose rows see all of the step
-    auto nan_rows = [&](int buffer, int step) {
+    auto nan_rows = [&](int buffer, int step) LFFN_INLINE {
         const int key0 = c0 + step * kManyKeys;
         const unsigned there = there_of(step);
         if (!edge(key0) && there == 15u) return;
@@ -768,31 +790,41 @@ __global__ __launch_bounds__(256, KIND != kElemF32 && DIM <= 128 ? 2 : 1) void a
         __builtin_amdgcn_sched_group_barrier(0x8, F, 0);
     };
 
-    uv2 ahead = {};         // the segment of the step whose bytes are on their way
-    if (steps > 0) {
-        ahead = segment(0);
-        fetch(0, ahead);
-        stage(0, 0, ahead);
-    }
-    __syncthreads();
-    for (int i = 0; i < steps; ++i) {
-        // (past the last step too, of block 0: with a branch around its loads, the waits in a step are for all of them)
-        ahead = segment(i + 1);
-        fetch(i + 1, ahead);
-        if (visible(c0 + i * kManyKeys)) {
-            scores(i & 1);
-            if constexpr (KIND != kElemF32) reads_ahead(std::integral_constant<int, FIRST>{}, std::integral_constant<int, DIM / 16 * T>{});
-            softmax(i);
-            __builtin_amdgcn_sched_barrier(0);
-            sums(i & 1);
-            if constexpr (KIND != kElemF32) reads_ahead(std::integral_constant<int, FIRST>{}, std::integral_constant<int, DIM / 16 * T>{});
-            nan_rows(i & 1, i);
+    auto run = [&](auto exactly) LFFN_INLINE {
+        constexpr bool EXACT = decltype(exactly)::value;
+        uv2 ahead = {};         // the segment of the step whose bytes are on their way
+        if (steps > 0) {
+            ahead = segment(0);
+            fetch(0, ahead);
+            stage(exactly, 0, 0, ahead);
         }
-        stage(~i & 1, i + 1, ahead);
         __syncthreads();
-    }
+        for (int i = 0; i < steps; ++i) {
+            // (past the last step too, of block 0: with a branch around its loads, the waits in a step are for all of them)
+            ahead = segment(i + 1);
+            fetch(i + 1, ahead);
+            if (visible(c0 + i * kManyKeys)) {
+                typename std::conditional_t<EXACT, XO, VO>::V p[2 * T][EXACT ? XP : NP];
+                scores(i & 1);
+                if constexpr (KIND != kElemF32) reads_ahead(std::integral_constant<int, FIRST>{}, std::integral_constant<int, DIM / 16 * T>{});
+                softmax(exactly, i, p);
+                __builtin_amdgcn_sched_barrier(0);
+                sums(exactly, i & 1, p);
+                if constexpr (KIND != kElemF32 && !EXACT) reads_ahead(std::integral_constant<int, FIRST>{}, std::integral_constant<int, DIM / 16 * T>{});
+                nan_rows(i & 1, i);
+            }
+            stage(exactly, ~i & 1, i + 1, ahead);
+            __syncthreads();
+        }
+    };
+    if (__builtin_expect(exact, false))
+        run(std::true_type{});
+    else
+        run(std::false_type{});
 
-    float total = l + __shfl_xor(l, 32), up = v_unit;
+    // (probabilities as they are from here on: chunks of both kinds are joined)
+    const float lift = exact ? 1.0f : __builtin_amdgcn_exp2f(-kProbUp), up = v_unit * lift;
+    float total = (l + __shfl_xor(l, 32)) * lift;
     if constexpr (KS > 1) {
         // the two waves of a row block: the later's sums go through LDS (whose steps are over) to the earlier
         float *from = reinterpret_cast<float *>(many_lds) + (w & 1) * (DIM / 2 + 2) * 64;

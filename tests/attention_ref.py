@@ -136,3 +136,16 @@ def attend_bound(y, size, reach, coarse_k, coarse_v, dtype, dim, most_keys):
     out = half_step(dtype) * y.abs() + (2.0 ** -25 if dtype == torch.float16 else 0.0)
     coarse = 0.0 if dtype == torch.float32 else 2.0 ** -25 * coarse_v[..., None]
     return out + (size * (2 * score + piece + 4 * U32 + 2 * sums) + coarse) * (1 + half_step(dtype))
+
+
+def attend_bound_rows(y, size, reach, dtype, dim, most_keys):
+    """As attend_bound, of rows that no block's scale touches but those they see: nothing is allowed for the largest scale of the request.
+
+    A rounding to half is off by half a step, 2^-11 of the value (the 2^-12 of attend_bound holds at the top of a binade only); two bf16 pieces are off by
+    less.  The matrix cores may take a product's factor below 2^-126 as zero, of up to 448 times each key, and fp32 holds no number below that
+    with all its bits."""
+    score = (dim + 9) * U32 * reach.double()[..., None]
+    piece = 2.0 ** -23 if dtype == torch.float32 else 2.0 ** -11
+    sums = (most_keys / 32 + 40) * U32
+    out = half_step(dtype) * y.abs() + (2.0 ** -25 if dtype == torch.float16 else 0.0)
+    return out + size * (2 * score + piece + 4 * U32 + 2 * sums) * (1 + half_step(dtype)) + 449 * most_keys * 2.0 ** -126
