@@ -329,8 +329,8 @@ int lookupffn_rotate_append(const void *q, const void *k, const void *v, const f
  * (0 .. lengths[r] - 1), where causal only up to the token's own position, where window > 0 only those fewer than `window` before it.
  * Query head h reads key head h * kv_heads / heads (heads a multiple of kv_heads).  A row that sees no key is zero, and a key whose block
  * is not in the cache (a table entry outside 0 .. n_blocks - 1, or past the table) is not seen.  Values and keys that a row does not see
- * do not reach it, whatever they hold.  max_queries and max_keys bound the tokens that a request brings and the lengths (what goes beyond
- * is left out); they shape the launch, so tight ones are faster.
+ * do not reach it, whatever they hold.  max_queries and max_keys bound the tokens that a request brings and the lengths: rows of
+ * tokens beyond are not written, keys beyond not seen.  They shape the launch, so tight ones are faster.
  * Sums, maximum and softmax are fp32; probabilities keep 11 bits or more (fp32 rows: 24) in the product with the values, those below 2^-22 of
  * the row's largest what 11 bits there keep (2^-33).  Scales may be any floats; powers of two at most 2^8 apart, as rotate_append writes them for
  * rows of like sizes, are the fastest.

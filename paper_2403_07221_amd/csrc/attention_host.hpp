@@ -201,9 +201,10 @@ AttendPlan plan_attend(int64_t n_tokens, int n_requests, int heads, int kv_heads
     p.many = rows > (dim == 64 ? 64 : 32);
     p.tile_rows = !p.many ? 16 : rows > 64 ? 128 : 64;
     p.row_tiles = (int)std::max<int64_t>((rows + p.tile_rows - 1) / p.tile_rows, 1);
-    // keys that a tile of rows can see, from a multiple of 64 on; where rows see what follows them, to the end of the request
+    // keys that a tile of rows can see, from a multiple of 64 on; where rows see what follows them, to the end of the request, which may bring
+    // more tokens than max_queries (the rows inside that bound see the others' keys)
     int64_t span = std::max<int64_t>(max_keys, 1);
-    if (window) span = std::min<int64_t>(span, (int64_t)window + (causal ? p.tile_rows : std::max<int64_t>(max_queries, p.tile_rows)) + 64);
+    if (window) span = std::min<int64_t>(span, (int64_t)window + (causal ? p.tile_rows : std::max<int64_t>(n_tokens, p.tile_rows)) + 64);
     span = (span + 63) / 64 * 64;
     const int64_t units = std::max<int64_t>((int64_t)n_requests * kv_heads * p.row_tiles, 1);
     // Chunks until the grid has 8 workgroups to a compute unit (many-row kernel: one and a half times what fits, as long as there are no

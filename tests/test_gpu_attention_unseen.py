@@ -7,7 +7,7 @@ import torch
 
 import attention_ref as R
 from paper_2403_07221_amd import binding as B
-from test_gpu_attention import DTYPES, make_attend, run_attend
+from test_gpu_attention import DTYPES, dev, make_attend, run_attend
 
 pytestmark = pytest.mark.gpu
 
@@ -18,10 +18,32 @@ def _gpu():
     B.lookupffn_init()
 
 
-def check_close(y, cache, table, starts, lengths, q, causal, window, take=None, lost=0.0):
+def dense(q, cache, table, starts, lengths, causal, window):
+    """R.attend's first three results for caches without NaN among the keys, a request's rows at once."""
+    heads, dim, (n_blocks, kv, block, _) = q.shape[1], q.shape[2], cache.k.shape
+    y, size, reach = torch.zeros(q.shape, dtype=torch.float64), torch.zeros(q.shape, dtype=torch.float64), torch.zeros(q.shape[:2])
+    for r, n in enumerate(lengths):
+        first, end = starts[r], starts[r + 1]
+        at = table[r][:-(-n // block)]
+        k = (cache.k[at].float().double() * cache.k_scale[at].double()[..., None, None]).transpose(0, 1).reshape(kv, -1, dim)[:, :n]
+        v = (cache.v[at].float().double() * cache.v_scale[at].double()[..., None, None]).permute(1, 0, 3, 2).reshape(kv, -1, dim)[:, :n]
+        where, j = torch.arange(n - (end - first), n)[:, None], torch.arange(n)[None]
+        hidden = (j > where) if causal else torch.zeros(where.shape[0], n, dtype=torch.bool)
+        if window:
+            hidden = hidden | (where - j >= window)
+        for h in range(heads):
+            x, kh, vh = q[first:end, h].double(), k[h * kv // heads], v[h * kv // heads]
+            p = torch.softmax((x @ kh.T / math.sqrt(dim)).masked_fill(hidden, -math.inf), 1)
+            y[first:end, h], size[first:end, h] = p @ vh, p @ vh.abs()
+            reach[first:end, h] = ((x.abs() @ kh.abs().T).masked_fill(hidden, 0).amax(1) / math.sqrt(dim)).float()
+    return y, size, reach
+
+
+def check_close(y, cache, table, starts, lengths, q, causal, window, take=None, lost=0.0, plain=None):
     """y against the 64-bit form, with no allowance for what other blocks' scales are; `take` picks rows.  lost: what each of a row's
     probabilities may be off by beside its own bits, relative to the row's largest."""
-    ref, size, reach = R.attend(q.cpu(), cache.k, cache.v, cache.k_scale, cache.v_scale, table, starts, lengths, causal, window)[:3]
+    ref, size, reach = (plain or R.attend)(q.cpu(), *((cache,) if plain else (cache.k, cache.v, cache.k_scale, cache.v_scale)), table, starts,
+                                           lengths, causal, window)[:3]
     bound = R.attend_bound_rows(ref, size, reach, q.dtype, q.shape[2], max(lengths))
     if lost:
         bound = bound + lost * max(lengths) * (448 * cache.v_scale[cache.v_scale.isfinite()].abs().max().double())
@@ -147,3 +169,22 @@ def test_scales_of_every_kind_in_several_chunks(fresh, dim, dtype):
         cache.v_scale[b] = (0.013, 0.0, 2.0 ** -7, -0.017, 2.0 ** -126, 1e-40)[i % 6]
     y = run_attend(cache, table, starts, [n], q)
     check_close(y, cache, table, starts, [n], q, True, 0, lost=2.0 ** -33 if dtype != torch.float32 else 0.0)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("heads,kv,dim,most", [(1, 1, 64, 3), (4, 4, 64, 40), (2, 2, 128, 70), (4, 1, 256, 10)])
+@pytest.mark.parametrize("window", [5, 100])
+def test_requests_that_bring_more_than_max_queries(window, heads, kv, dim, most, dtype):
+    """The rows inside the bound see all their keys, the others are not written."""
+    lengths, fresh = [1400, 900, 70], [1000, 2, 60]
+    print("more", window, heads, kv, dim, most, dtype, flush=True)
+    cache, table, starts, q = make_attend(9, lengths, fresh, heads, kv, dim, 64, dtype)
+    inside = torch.zeros(starts[-1], dtype=torch.bool)
+    for a, b in zip(starts, starts[1:]):
+        inside[a:min(b, a + most)] = True
+    for causal in (True, False):
+        y = torch.full_like(q, 7.0, memory_format=torch.contiguous_format)
+        B.lookupffn_attend(q, *cache.on_gpu(), dev(table), dev(starts), dev(lengths), y=y, causal=causal, window=window, max_queries=most,
+                           max_keys=max(lengths))
+        assert (y[~inside.cuda()] == 7).all()
+        check_close(y, cache, table, starts, lengths, q, causal, window, take=inside, plain=dense)
