@@ -21,7 +21,8 @@ struct AttendArgs {
     int n_tokens, requests, heads, kv_heads, group;
     unsigned group_inverse;   // floor(2^32 / group), for group > 1
     int width, n_blocks, block_log;
-    int causal, window, max_keys;
+    int causal, window;
+    int max_keys;         // of a request: what the caller says, and what a row of the table holds
     int max_queries;      // tokens of a request that the grid (and the few-row kernel's LDS) has room for
     int chunk, chunks;    // keys of a chunk, chunks of the grid
     int row_tiles;        // tiles of rows of a request and key head, of the grid
@@ -54,16 +55,14 @@ LFFN_TILE RowTile row_tile(const AttendArgs &a, int combo, int tile, int tile_ro
     t.h = combo - t.r * a.kv_heads;
     t.first = min(max(a.starts[t.r], 0), a.n_tokens);
     t.fresh = min(max(a.starts[t.r + 1], t.first), a.n_tokens) - t.first;
-    const int whole = max(a.lengths[t.r], 0), blocks = min(a.width, (a.max_keys >> a.block_log) + 1);
-    const int length = min(whole, min(a.max_keys, blocks << a.block_log));
+    const int whole = max(a.lengths[t.r], 0), length = min(whole, a.max_keys);
     t.past = whole - t.fresh;
     t.rows = min(t.fresh, a.max_queries) * a.group;
     t.row0 = tile * tile_rows;
-    t.lo = t.hi = 0;
-    if (t.row0 >= t.rows) return t;
-    const int i0 = query_of(a, t.row0), i1 = query_of(a, min(t.row0 + tile_rows, t.rows) - 1);
-    t.hi = a.causal ? min(length, max(t.past + i1, -1) + 1) : length;   // (past + i1 is below `whole`)
-    t.lo = a.window ? max(t.past + i0 - a.window + 1, 0) : 0;
+    const int last = max(min(t.row0 + tile_rows, t.rows) - 1, 0);
+    const int p0 = t.past + query_of(a, min(t.row0, last)), p1 = t.past + query_of(a, last);   // positions of the first and the last row
+    t.hi = a.causal && p1 < length ? max(p1, -1) + 1 : length;
+    t.lo = a.window ? max(p0 - a.window + 1, 0) : 0;
     t.lo = min(t.lo, t.hi) & ~63;   // chunks and steps begin at multiples of 64 keys
     return t;
 }

@@ -310,7 +310,7 @@ int attend(const void *q, const void *k_cache, const void *v_cache, const float 
     a.block_log = log2_of(block);
     a.causal = causal != 0;
     a.window = window;
-    a.max_keys = (int)max_keys;
+    a.max_keys = (int)std::min<int64_t>(max_keys, (int64_t)table_width * block);
     a.max_queries = (int)max_queries;
     a.chunk = p.chunk;
     a.chunks = p.chunks;

@@ -108,7 +108,7 @@ int main()
                                     a.n_tokens = a.max_queries = n;
                                     a.window = window;
                                     a.causal = causal;
-                                    a.max_keys = max_keys;
+                                    a.max_keys = (int)std::min<long long>(max_keys, (long long)width << block_log);   // as attend() does
                                     a.block_log = block_log;
                                     a.width = width;
                                     a.n_blocks = 10;
