@@ -284,7 +284,7 @@ int64_t lookupffn_workspace_bytes_bh_weighted(int64_t n_tokens, int d, int k, in
  * [n_blocks][kv_heads][dim][block] e4m3 bytes, 16-byte aligned; k_scale and v_scale [n_blocks][kv_heads] fp32: a byte b stands for
  * b * scale.  A slot is block * (tokens of a block) + place.  table [n_requests][table_width] int32 (rows table_stride apart) names the
  * blocks of a request in order.  No content of a table, slot, position or length makes a kernel access memory outside its arguments.
- * At most 2^30 tokens, 2^31 - 1 tokens times heads, 4096 heads.
+ * At most 2^30 tokens, 4096 heads, and in attention 2^31 - 256 tokens times heads.
  *
  * lookupffn_plan_cache: request r has past[r] tokens in the cache and brings fresh[r] (negative counts are zero).  Writes
  *   starts[n_requests + 1]  exclusive sums of fresh;  lengths[r] = past[r] + fresh[r];

@@ -4,7 +4,7 @@
 bool block_ok(int block) { return block == 16 || block == 32 || block == 64 || block == 128; }
 int log2_of(int block) { return __builtin_ctz((unsigned)block); }
 constexpr int64_t kMaxStepTokens = int64_t(1) << 30;
-constexpr int64_t kMaxRows = (int64_t(1) << 31) - 1;   // tokens * heads
+constexpr int64_t kMaxRows = (int64_t(1) << 31) - 256;   // tokens * heads: a tile's rows past the last one are ints too
 constexpr int kMaxHeads = 4096;
 
 // ---------------------------------------------------------------- plan

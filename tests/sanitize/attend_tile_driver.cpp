@@ -64,6 +64,7 @@ static void one(AttendArgs a, int start, int end, int length, int tile_rows)
         if (tile * (long long)tile_rows >= rows) continue;
         const RowTile t = row_tile(a, 0, tile, tile_rows);
         ++cases;
+        if (t.row0 + (long long)tile_rows + 128 > INT32_MAX) fail("a row past the tile", a, t.row0);   // (waves and the join count on past the last)
         if (t.row0 >= t.rows) continue;
         if (t.lo < 0 || t.lo > t.hi || t.hi > a.max_keys || t.lo % 64) fail("the tile's keys", a, t.lo);
         // the definition, in 64 bits
@@ -94,8 +95,8 @@ int main()
     AttendArgs a{};
     a.kv_heads = 1;
     a.requests = 1;
-    for (int group : {1, 3, 8})
-        for (int n : {1, 5, 300, big / group})
+    for (int group : {1, 2, 3, 8})
+        for (int n : {1, 5, 300, big / group, (int)std::min<long long>(big, ((1LL << 31) - 256) / group)})
             for (int window : {0, 1, 2, 63, 64, 190, 2000, 100000, big})
                 for (int causal : {0, 1})
                     for (int max_keys : {0, 1, 64, 1000, 131072, big})

@@ -7,6 +7,8 @@ from pathlib import Path
 
 import pytest
 
+from paper_2403_07221_amd import binding
+
 ROOT = Path(__file__).resolve().parent.parent
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 CLANG = "/opt/rocm/lib/llvm/bin/clang++"
@@ -24,3 +26,16 @@ def test_tiles_of_any_lengths(tmp_path):
         assert p.returncode == 0, p.stdout[-3000:]
     p = subprocess.run([str(exe)], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=300)
     assert p.returncode == 0 and "ran clean" in p.stdout and "runtime error" not in p.stdout, p.stdout[-3000:]
+
+
+def test_the_most_rows():
+    """What the driver takes as the most rows is what attention refuses to go beyond (a type that is none tells what is looked at after)."""
+    L, fake = binding.lib(), 1 << 20
+
+    def attend(n, heads, kv):
+        return L.lookupffn_attend(fake, fake, fake, fake, fake, fake, fake, fake, fake, n, 1, heads, kv, 64, 7, 16, 2, 2, None, n, 32, 1, 0, 3, None, 0, None)
+
+    most = (1 << 31) - 256
+    for heads in (2, 4, 8):
+        assert attend(most // heads, heads, 2) == -4 and attend(most // heads + 1, heads, 2) == -2
+    assert attend(1 << 30, 1, 1) == -4 and attend((1 << 30) + 1, 1, 1) == -2
