@@ -56,15 +56,17 @@ void of_type(const Tensor &t, const char *name, at::ScalarType type)
 {
     if (t.scalar_type() != type) fail(PyExc_TypeError, "%s must be %s, got %s", name, c10::toString(type), c10::toString(t.scalar_type()));
 }
-void *on_gpu(const Tensor &t, const char *name)
+// `home`: the call's device, where its first tensor is
+void *on_gpu(const Tensor &t, const char *name, at::Device home)
 {
     if (!t.is_cuda()) fail(PyExc_ValueError, "%s must live on the GPU", name);
+    if (t.device() != home) fail(PyExc_ValueError, "%s lives on %s, the call's device is %s", name, t.device().str().c_str(), home.str().c_str());
     return t.data_ptr();
 }
-void *dense(const Tensor &t, const char *name)
+void *dense(const Tensor &t, const char *name, at::Device home)
 {
     if (!t.is_contiguous()) fail(PyExc_ValueError, "%s must be contiguous", name);
-    return on_gpu(t, name);
+    return on_gpu(t, name, home);
 }
 void shaped(const Tensor &t, const char *name, at::IntArrayRef shape)
 {
@@ -74,18 +76,18 @@ void shaped(const Tensor &t, const char *name, at::IntArrayRef shape)
     for (int64_t v : shape) want += (want.empty() ? "" : ", ") + std::to_string(v);
     fail(PyExc_ValueError, "%s has shape (%s), expected (%s)", name, got.c_str(), want.c_str());
 }
-void *ints(const Tensor &t, const char *name, at::IntArrayRef shape)
+void *ints(const Tensor &t, const char *name, at::IntArrayRef shape, at::Device home)
 {
     of_type(t, name, at::kInt);
     shaped(t, name, shape);
-    return dense(t, name);
+    return dense(t, name, home);
 }
 // rows [tokens][heads][dim] of any strides, columns dense
-void *rows(const Tensor &t, const char *name, at::IntArrayRef shape, at::ScalarType type)
+void *rows(const Tensor &t, const char *name, at::IntArrayRef shape, at::ScalarType type, at::Device home)
 {
     of_type(t, name, type);
     shaped(t, name, shape);
-    void *p = on_gpu(t, name);
+    void *p = on_gpu(t, name, home);
     if (t.stride(2) != 1) fail(PyExc_ValueError, "the columns of %s must be dense", name);
     return p;
 }
@@ -98,12 +100,12 @@ int dtype_code(const Tensor &t)
         default: fail(PyExc_TypeError, "expected float32, bfloat16 or float16, got %s", c10::toString(t.scalar_type()));
     }
 }
-void *row_weight(const Tensor &w, const char *name, int64_t dim)
+void *row_weight(const Tensor &w, const char *name, int64_t dim, at::Device home)
 {
     if (!w.defined()) return nullptr;
     of_type(w, name, at::kFloat);
     shaped(w, name, {dim});
-    return dense(w, name);
+    return dense(w, name, home);
 }
 void three(const Tensor &t, const char *name)
 {
@@ -153,14 +155,14 @@ struct Rotation {
     const void *angles = nullptr, *positions = nullptr;
     int rot = 0;
     int64_t n_positions = 0;
-    Rotation(PyObject *a, PyObject *p, int64_t n)
+    Rotation(PyObject *a, PyObject *p, int64_t n, at::Device home)
     {
         if (a == Py_None) return;
         const Tensor &t = tensor(a, "angles");
         if (t.scalar_type() != at::kFloat || t.dim() != 2) fail(PyExc_TypeError, "angles must be float32 [positions][rot]");
         if (p == Py_None) fail(PyExc_ValueError, "angles need positions");
-        angles = dense(t, "angles");
-        positions = ints(tensor(p, "positions"), "positions", {n});
+        angles = dense(t, "angles", home);
+        positions = ints(tensor(p, "positions"), "positions", {n}, home);
         rot = (int)t.size(1);
         n_positions = t.size(0);
     }
@@ -170,7 +172,8 @@ struct Cache {
     int64_t n_blocks;
     int block;
     void *k, *v, *ks, *vs;
-    Cache(const Tensor &kc, const Tensor &vc, const Tensor &k_scale, const Tensor &v_scale, int64_t kv_heads, int64_t dim)
+    Cache(const Tensor &kc, const Tensor &vc, const Tensor &k_scale, const Tensor &v_scale, int64_t kv_heads, int64_t dim,
+          at::Device home)
     {
         of_type(kc, "k_cache", at::kFloat8_e4m3fn);
         of_type(vc, "v_cache", at::kFloat8_e4m3fn);
@@ -184,10 +187,10 @@ struct Cache {
         shaped(k_scale, "k_scale", {n_blocks, kv_heads});
         shaped(v_scale, "v_scale", {n_blocks, kv_heads});
         block = (int)b;
-        k = dense(kc, "k_cache");
-        v = dense(vc, "v_cache");
-        ks = dense(k_scale, "k_scale");
-        vs = dense(v_scale, "v_scale");
+        k = dense(kc, "k_cache", home);
+        v = dense(vc, "v_cache", home);
+        ks = dense(k_scale, "k_scale", home);
+        vs = dense(v_scale, "v_scale", home);
     }
 };
 
@@ -210,17 +213,18 @@ PyObject *plan_cache(PyObject *const *a)
         fail(PyExc_TypeError, "table must be int32 [%lld][blocks of a request]", (long long)requests);
     if (free.dim() != 1) fail(PyExc_ValueError, "free must be a list of blocks");
     if (n_tokens < 0) fail(PyExc_ValueError, "n_tokens must not be negative");
-    void *p_past = ints(past, "past", {requests}), *p_fresh = ints(fresh, "fresh", {requests}), *p_free = ints(free, "free", {free.size(0)});
-    void *p_table = ints(table, "table", {requests, table.size(1)});
+    const at::Device home = past.device();
+    void *p_past = ints(past, "past", {requests}, home), *p_fresh = ints(fresh, "fresh", {requests}, home);
+    void *p_free = ints(free, "free", {free.size(0)}, home), *p_table = ints(table, "table", {requests, table.size(1)}, home);
     const char *names[5] = {"starts", "lengths", "slots", "positions", "counts"};
     const int64_t sizes[5] = {requests + 1, requests, n_tokens, n_tokens, 2};
     Tensor out[5];
     void *p[5];
     for (int i = 0; i < 5; ++i) {
         out[i] = a[6 + i] == Py_None ? at::empty({sizes[i]}, past.options()) : tensor(a[6 + i], names[i]);
-        p[i] = ints(out[i], names[i], {sizes[i]});
+        p[i] = ints(out[i], names[i], {sizes[i]}, home);
     }
-    const c10::DeviceGuard guard(past.device());
+    const c10::DeviceGuard guard(home);
     checked(g_plan(p_past, p_fresh, p_free, p_table, p[0], p[1], p[2], p[3], p[4], (int)requests, free.size(0), (int)table.size(1),
                    table.size(1), n_tokens, small(a[5]), stream_of(past)));
     return tuple_of({out[0], out[1], out[2], out[3], out[4]});
@@ -235,17 +239,18 @@ PyObject *rotate(PyObject *const *a)
     const int64_t n = q.size(0), heads = q.size(1), dim = q.size(2), kv = k.size(1);
     const at::ScalarType type = q.scalar_type();
     const int code = dtype_code(q);
-    void *pq = rows(q, "q", {n, heads, dim}, type), *pk = rows(k, "k", {n, kv, dim}, type);
-    void *qw = row_weight(maybe(a[2], "q_weight"), "q_weight", dim), *kw = row_weight(maybe(a[3], "k_weight"), "k_weight", dim);
-    const Rotation r(a[4], a[5], n);
+    const at::Device home = q.device();
+    void *pq = rows(q, "q", {n, heads, dim}, type, home), *pk = rows(k, "k", {n, kv, dim}, type, home);
+    void *qw = row_weight(maybe(a[2], "q_weight"), "q_weight", dim, home), *kw = row_weight(maybe(a[3], "k_weight"), "k_weight", dim, home);
+    const Rotation r(a[4], a[5], n, home);
     const Tensor qo = a[6] == Py_None ? at::empty({n, heads, dim}, q.options()) : tensor(a[6], "q_out");
     const Tensor ko = a[7] == Py_None ? at::empty({n, kv, dim}, q.options()) : tensor(a[7], "k_out");
-    void *pqo = rows(qo, "q_out", {n, heads, dim}, type), *pko = rows(ko, "k_out", {n, kv, dim}, type);
+    void *pqo = rows(qo, "q_out", {n, heads, dim}, type, home), *pko = rows(ko, "k_out", {n, kv, dim}, type, home);
     if (n) {
         const int64_t strides[8] = {q.stride(0), q.stride(1), k.stride(0), k.stride(1), qo.stride(0), qo.stride(1), ko.stride(0), ko.stride(1)};
         const double eps = PyFloat_AsDouble(a[8]);
         if (eps == -1.0 && PyErr_Occurred()) throw PythonError();
-        const c10::DeviceGuard guard(q.device());
+        const c10::DeviceGuard guard(home);
         checked(g_rotate(pq, pk, qw, kw, r.angles, r.positions, pqo, pko, n, (int)heads, (int)kv, (int)dim, r.rot, r.n_positions, strides,
                          (float)eps, truth(a[9]), code, stream_of(q)));
     }
@@ -261,18 +266,19 @@ PyObject *rotate_append(PyObject *const *a)
     const int64_t n = q.size(0), heads = q.size(1), dim = q.size(2), kv = k.size(1);
     const at::ScalarType type = q.scalar_type();
     const int code = dtype_code(q);
-    void *pq = rows(q, "q", {n, heads, dim}, type), *pk = rows(k, "k", {n, kv, dim}, type), *pv = rows(v, "v", {n, kv, dim}, type);
-    void *qw = row_weight(maybe(a[3], "q_weight"), "q_weight", dim), *kw = row_weight(maybe(a[4], "k_weight"), "k_weight", dim);
-    const Rotation r(a[5], a[6], n);
-    void *slots = ints(tensor(a[7], "slots"), "slots", {n});
-    const Cache c(tensor(a[8], "k_cache"), tensor(a[9], "v_cache"), tensor(a[10], "k_scale"), tensor(a[11], "v_scale"), kv, dim);
+    const at::Device home = q.device();
+    void *pq = rows(q, "q", {n, heads, dim}, type, home), *pk = rows(k, "k", {n, kv, dim}, type, home), *pv = rows(v, "v", {n, kv, dim}, type, home);
+    void *qw = row_weight(maybe(a[3], "q_weight"), "q_weight", dim, home), *kw = row_weight(maybe(a[4], "k_weight"), "k_weight", dim, home);
+    const Rotation r(a[5], a[6], n, home);
+    void *slots = ints(tensor(a[7], "slots"), "slots", {n}, home);
+    const Cache c(tensor(a[8], "k_cache"), tensor(a[9], "v_cache"), tensor(a[10], "k_scale"), tensor(a[11], "v_scale"), kv, dim, home);
     const Tensor qo = a[12] == Py_None ? at::empty({n, heads, dim}, q.options()) : tensor(a[12], "q_out");
-    void *pqo = rows(qo, "q_out", {n, heads, dim}, type);
+    void *pqo = rows(qo, "q_out", {n, heads, dim}, type, home);
     if (n) {
         const int64_t strides[8] = {q.stride(0), q.stride(1), k.stride(0), k.stride(1), v.stride(0), v.stride(1), qo.stride(0), qo.stride(1)};
         const double eps = PyFloat_AsDouble(a[13]);
         if (eps == -1.0 && PyErr_Occurred()) throw PythonError();
-        const c10::DeviceGuard guard(q.device());
+        const c10::DeviceGuard guard(home);
         checked(g_append(pq, pk, pv, qw, kw, r.angles, r.positions, slots, pqo, c.k, c.v, c.ks, c.vs, n, (int)heads, (int)kv, (int)dim, r.rot,
                          r.n_positions, c.n_blocks, c.block, strides, (float)eps, truth(a[14]), code, stream_of(q)));
     }
@@ -291,19 +297,20 @@ PyObject *attend(PyObject *const *a)
         fail(PyExc_ValueError, "table must be [%lld][blocks of a request]", (long long)requests);
     const at::ScalarType type = q.scalar_type();
     const int code = dtype_code(q);
-    void *pq = rows(q, "q", {n, heads, dim}, type);
+    const at::Device home = q.device();
+    void *pq = rows(q, "q", {n, heads, dim}, type, home);
     const Tensor y = a[8] == Py_None ? at::empty({n, heads, dim}, q.options()) : tensor(a[8], "y");
-    void *py = rows(y, "y", {n, heads, dim}, type);
-    const Cache c(kc, tensor(a[2], "v_cache"), tensor(a[3], "k_scale"), tensor(a[4], "v_scale"), kv, dim);
-    void *pt = ints(table, "table", {requests, table.size(1)}), *ps = ints(tensor(a[6], "starts"), "starts", {requests + 1});
-    void *pl = ints(lengths, "lengths", {requests});
+    void *py = rows(y, "y", {n, heads, dim}, type, home);
+    const Cache c(kc, tensor(a[2], "v_cache"), tensor(a[3], "k_scale"), tensor(a[4], "v_scale"), kv, dim, home);
+    void *pt = ints(table, "table", {requests, table.size(1)}, home);
+    void *ps = ints(tensor(a[6], "starts"), "starts", {requests + 1}, home), *pl = ints(lengths, "lengths", {requests}, home);
     if (n) {
         const int64_t max_queries = a[11] == Py_None ? n : whole(a[11]);
         const int64_t max_keys = a[12] == Py_None ? table.size(1) * c.block : whole(a[12]);
         const Tensor ws = maybe(a[13], "workspace");
-        void *pw = ws.defined() ? dense(ws, "workspace") : nullptr;
+        void *pw = ws.defined() ? dense(ws, "workspace", home) : nullptr;
         const int64_t strides[4] = {q.stride(0), q.stride(1), y.stride(0), y.stride(1)};
-        const c10::DeviceGuard guard(q.device());
+        const c10::DeviceGuard guard(home);
         checked(g_attend(pq, c.k, c.v, c.ks, c.vs, pt, ps, pl, py, n, (int)requests, (int)heads, (int)kv, (int)dim, c.n_blocks, c.block,
                          (int)table.size(1), table.size(1), strides, max_queries, max_keys, truth(a[9]), small(a[10]), code, pw,
                          ws.defined() ? (int64_t)ws.nbytes() : 0, stream_of(q)));
