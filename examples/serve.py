@@ -79,14 +79,19 @@ class Server:
         self.past = [0] * requests
 
     def step(self, x: torch.Tensor, fresh: list[int]) -> torch.Tensor:
-        """x[sum of fresh, d], the new tokens request by request, through all layers; their keys and values stay in the cache."""
+        """x[sum of fresh, d], the new tokens request by request, through all layers; their keys and values stay in the cache.  A step that
+        does not fit is refused before anything changes."""
+        if len(fresh) != len(self.past) or min(fresh) < 0 or sum(fresh) != x.shape[0]:
+            raise ValueError(f"{len(self.past)} requests bring {fresh}: {x.shape[0]} tokens")
+        if max(p + f for p, f in zip(self.past, fresh)) > self.angles.shape[0]:
+            raise ValueError(f"a request would be longer than {self.angles.shape[0]} tokens")
+        taken = sum(-(-(p + f) // self.block) - -(-p // self.block) for p, f in zip(self.past, fresh))
+        if taken > self.free.numel():
+            raise ValueError("the cache has too few blocks left")
         s = Step()
         past = torch.tensor(self.past, dtype=torch.int32, device="cuda")
         s.starts, s.lengths, s.slots, s.positions, _ = B.lookupffn_plan_cache(
             past, torch.tensor(fresh, dtype=torch.int32, device="cuda"), self.free, self.table, x.shape[0], self.block)
-        taken = sum(-(-(p + f) // self.block) - -(-p // self.block) for p, f in zip(self.past, fresh))
-        if taken > self.free.numel():
-            raise ValueError("the cache has too few blocks left")
         self.free = self.free[taken:]
         self.past = [p + f for p, f in zip(self.past, fresh)]
         s.table, s.angles, s.max_queries, s.max_keys = self.table, self.angles, max(fresh), max(self.past)
