@@ -188,3 +188,26 @@ def test_requests_that_bring_more_than_max_queries(window, heads, kv, dim, most,
                            max_keys=max(lengths))
         assert (y[~inside.cuda()] == 7).all()
         check_close(y, cache, table, starts, lengths, q, causal, window, take=inside, plain=dense)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("fresh", [2, 80])
+@pytest.mark.parametrize("window", [0, 1010])
+def test_keys_past_the_table_are_not_there(fresh, window, dtype):
+    """A request longer than its row of the table: all slots of its last block are keys, and no more."""
+    cache, table, starts, q = make_attend(7, [fresh], [fresh], 4, 4, 64, 16, dtype)
+    without_nan(cache)
+    cut, lengths = [row[:-(-fresh // 16)] for row in table], [fresh + 1000]
+    y = B.lookupffn_attend(q, *cache.on_gpu(), dev(cut), dev(starts), dev(lengths), window=window, max_queries=fresh, max_keys=fresh + 1000)
+    check_close(y, cache, cut, starts, lengths, q, True, window)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("heads,kv,dim", [(8, 4, 64), (8, 2, 128), (4, 2, 256)])
+def test_rows_are_the_same_every_time(heads, kv, dim, dtype):
+    """No sum's order depends on what runs when."""
+    lengths, fresh = [1400, 37, 900, 3], [300, 37, 20, 3]
+    cache, table, starts, q = make_attend(11, lengths, fresh, heads, kv, dim, 32, dtype)
+    on, ints = cache.on_gpu(), [dev(table), dev(starts), dev(lengths)]
+    y = [B.lookupffn_attend(q, *on, *ints, max_queries=300, max_keys=1400) for _ in range(6)]
+    assert all(torch.equal(y[0], other) for other in y[1:])
