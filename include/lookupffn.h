@@ -291,8 +291,8 @@ int64_t lookupffn_workspace_bytes_bh_weighted(int64_t n_tokens, int d, int k, in
  *   positions[n_tokens], slots[n_tokens]  of each token, request after request: past[r], past[r] + 1, ...;
  *   counts[2]  blocks taken off the front of free_blocks[n_free], and the sum of fresh;
  *   table  the columns of new blocks (ceil(past / block) ..), in place.
- * Slot -1: the step has no such token (n_tokens > counts[1]; position 0), the free blocks or the table's columns do not reach it, or its
- * block is negative; the later calls pass over it.  Tokens past n_tokens are not placed.  Sums stop at 2^31 - 1.  Up to 8000 requests.
+ * Slot -1: the step has no such token (n_tokens > counts[1]) or the table's columns do not reach it (position 0 in both), the free blocks do
+ * not reach it (its column stays as it is), or its block is negative; the later calls pass over it.  Tokens past n_tokens are not placed.  Sums stop at 2^31 - 1.  Up to 8000 requests.
  */
 int lookupffn_plan_cache(const int32_t *past, const int32_t *fresh, const int32_t *free_blocks, int32_t *table, int32_t *starts,
                          int32_t *lengths, int32_t *slots, int32_t *positions, int32_t *counts, int n_requests, int64_t n_free,
@@ -316,7 +316,7 @@ int lookupffn_rotate(const void *q, const void *k, const float *q_weight, const 
  * before those written are rounded once more to the new one.  Bytes are round to nearest even; NaN and infinities are stored as NaN.
  * Tokens that share a block have to follow one another in the step, in consecutive slots, as lookupffn_plan_cache places them (else what
  * the block holds is any of several results); tokens with slots outside the cache are passed over.  The bytes of other slots stay.
- * strides: q, k, v, q_out.  dim a multiple of 16 up to 256.
+ * strides: q, k, v, q_out.  dim a multiple of 16 up to 256 (lookupffn_attend reads caches of 64, 128, 192 and 256).
  */
 int lookupffn_rotate_append(const void *q, const void *k, const void *v, const float *q_weight, const float *k_weight, const float *angles,
                             const int32_t *positions, const int32_t *slots, void *q_out, void *k_cache, void *v_cache, float *k_scale,
@@ -329,12 +329,13 @@ int lookupffn_rotate_append(const void *q, const void *k, const void *v, const f
  * (0 .. lengths[r] - 1), where causal only up to the token's own position, where window > 0 only those fewer than `window` before it.
  * Query head h reads key head h * kv_heads / heads (heads a multiple of kv_heads).  A row that sees no key is zero, and a key whose block
  * is not in the cache (a table entry outside 0 .. n_blocks - 1, or past the table) is not seen.  Values and keys that a row does not see
- * do not reach it, whatever they hold.  max_queries and max_keys bound the tokens that a request brings and the lengths: rows of
- * tokens beyond are not written, keys beyond not seen.  They shape the launch, so tight ones are faster.
+ * do not reach it, whatever they hold.  max_queries and max_keys bound the tokens that a request brings and the lengths: rows of tokens
+ * beyond are not written, keys beyond not seen.  They shape the launch, so tight ones are faster.  Nor are rows written of tokens that
+ * belong to no request.
  * Sums, maximum and softmax are fp32; probabilities keep 11 bits or more (fp32 rows: 24) in the product with the values, those below 2^-22 of
  * the row's largest what 11 bits there keep (2^-33).  Scales may be any floats; powers of two at most 2^8 apart, as rotate_append writes them for
  * rows of like sizes, are the fastest.
- * strides: q, y.  dim 64, 128, 192 or 256.  Scratch: lookupffn_workspace_bytes_attend() bytes (0: the call needs none).
+ * strides: q, y.  dim 64, 128, 192 or 256.  Scratch: lookupffn_workspace_bytes_attend() bytes, enough causal or not (0: the call needs none).
  */
 int lookupffn_attend(const void *q, const void *k_cache, const void *v_cache, const float *k_scale, const float *v_scale,
                      const int32_t *table, const int32_t *starts, const int32_t *lengths, void *y, int64_t n_tokens, int n_requests,

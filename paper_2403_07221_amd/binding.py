@@ -622,7 +622,7 @@ def lookupffn_attend(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tens
                      workspace: torch.Tensor | None = None) -> torch.Tensor:
     """y[n, heads, dim]: attention of q[n, heads, dim] over the 8-bit cache (softmax of q k / sqrt(dim) over the keys a row sees).
     max_queries / max_keys: the most tokens a request brings / the longest request, where the caller knows them (default: what the
-    shapes allow)."""
+    shapes allow).  Rows of tokens that belong to no request are not written: in a y made here they hold anything."""
     return (_marshal or _native()).attend(q, k_cache, v_cache, k_scale, v_scale, table, starts, lengths, y, causal, window, max_queries,
                                           max_keys, workspace)
 

@@ -388,7 +388,7 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 2 : 1) void attend_few_kernel(Att
 
 // Many rows: prompts and encodings.  A workgroup has 128 rows of one request and key head, a wave 32 (KS = 2: 64, and of a step's two tiles
 // of 32 keys each wave has one; two waves join at the end); its keys go through LDS in steps of 64, widened to the matrix cores' type once
-// for all four waves.  Measured: 4 prompts of 3500 to 4096 tokens, 32 heads on 8 of 128, 600 us, 810 TFLOP/s; 64 encodings of 300 to 512,
+// for all four waves.  Measured: 4 prompts of 3500 to 4096 tokens, 32 heads on 8 of 128, 594 to 611 us, 800 to 820 TFLOP/s; 64 encodings of 300 to 512,
 // 12 heads of 64, 77 us, 460 TFLOP/s; 24 requests with 3 to 8 drafted tokens, 16 heads on 2 of 256 (KS = 2), 46 us, 1.2 TB/s.
 //
 // What bounds it: the matrix cores, and beside them the softmax's vector instructions.  Scores are S^T = K Q^T in tiles of 32 keys x 32
@@ -404,7 +404,7 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 2 : 1) void attend_few_kernel(Att
 // A chunk with a scale that is no power of two, or with scales further apart, is `exact`: its bytes stay as they are, a block's scale
 // multiplies its fp32 scores or its fp32 probabilities, and those are two bf16 pieces (16-bit rows), as in the few-row kernel.  So no block's
 // scale costs the bits of another's bytes, and nothing of a block reaches a row that does not see it.  All of its steps cost what that takes:
-// the prompts above 1010 us, the encodings 153, the drafted tokens 58.
+// the prompts above 1012 to 1022 us, the encodings 153, the drafted tokens 58.
 constexpr int kManyKeys = 64;
 constexpr float kProbUp = 8.0f;   // probabilities times 2^8
 // Scales of a chunk lie at most 2^8 apart: 8192 probabilities off by 2^-33 each, of values 2^8 times the row's others, are then no more than
