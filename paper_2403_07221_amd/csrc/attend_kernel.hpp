@@ -302,7 +302,8 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 2 : 1) void attend_few_kernel(Att
         }
         l += sum;
         // A masked key's probability is zero, but zero times a NaN byte is not: in masked steps such bytes become zeros, and
-        // the rows that do see one get their NaN from a product with ones in its place.
+        // the rows that do see one get their NaN from a product with ones in its place.  (A seen key whose probability is too small for
+        // bf16 takes the smallest in such a step.)
         bool nans = false;
         if (masked) {
             unsigned any = 0;
@@ -310,7 +311,20 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 2 : 1) void attend_few_kernel(Att
             for (int d = 0; d < D; ++d) any |= nan_bytes(vr[d][0]) | nan_bytes(vr[d][1]) | nan_bytes(vr[d][2]) | nan_bytes(vr[d][3]);
             nans = __any(any != 0);
         }
-        if (nans) {
+        if (__builtin_expect(nans, false)) {
+            // (bit e: whether the row sees key 16 g + e of the step; anew, or the masks of all sixteen scores are kept until here)
+            const int at = key0 + 16 * g, from = min(max(key_lo - at, 0), 16), to = valid ? min(max(min(key_hi, c1) - at, 0), 16) : 0;
+            const unsigned seen = ((1u << to) - 1) & (~0u << from);
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                uv4 words = __builtin_bit_cast(uv4, p[u][0]);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const unsigned shift = 16 * (e & 1), small = (words[e >> 1] >> shift & 0x7F80u) == 0;
+                    words[e >> 1] |= (seen >> (8 * u + e) & small) << (7 + shift);   // 2^-126
+                }
+                p[u][0] = __builtin_bit_cast(bf8, words);
+            }
 #pragma unroll
             for (int d = 0; d < D; ++d) {
                 uv4 ones;

@@ -211,3 +211,21 @@ def test_rows_are_the_same_every_time(heads, kv, dim, dtype):
     on, ints = cache.on_gpu(), [dev(table), dev(starts), dev(lengths)]
     y = [B.lookupffn_attend(q, *on, *ints, max_queries=300, max_keys=1400) for _ in range(6)]
     assert all(torch.equal(y[0], other) for other in y[1:])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("fresh,dim", [(1, 64), (5, 64), (2, 128), (1, 256), (70, 64), (40, 128)])
+def test_nan_values_without_weight(fresh, dim, dtype):
+    """A NaN value reaches the rows that see it also where its probability is too small for any type."""
+    n, heads, kv = 150, 4, 2
+    print("nan without weight", fresh, dim, dtype, flush=True)
+    for key in (20, n - fresh, 140):
+        if key > n - fresh:
+            continue
+        cache, table, starts, q = make_attend(12, [n], [fresh], heads, kv, dim, 16, dtype)
+        q.copy_(torch.ones_like(q))
+        at = table[0][key // 16]
+        cache.k[at, 0, key % 16], cache.k_scale[at, 0] = -448.0, 1.0     # a score of -448 sqrt(dim)
+        cache.v[at, 0, 3, key % 16] = math.nan
+        hit = run_attend(cache, table, starts, [n], q).cpu().isnan()
+        assert hit[:, :2, 3].all() and int(hit.sum()) == 2 * fresh, key
